@@ -464,7 +464,8 @@ park_status park_cache_workspace_size(const park_kv_cache* cache, const park_att
  * sequence b stands at position lens[b] - q_lens[b] + i.  dims: B, Hq, Hkv, Nq
  * and d; dtype must be PARK_BF16, Nk is not read.  opts: q_pos is not read,
  * q_doc and k_doc must be NULL.  Rows i >= q_lens[b] of O and lse are left as
- * they were.  Tokens on pages that are not valid are left out. */
+ * they were.  Tokens on pages that are not valid, and those past max_pages,
+ * are left out. */
 park_status park_cache_attention(const park_rows* Q, const park_kv_cache* cache,
                                  const int32_t* block_table, int32_t max_pages,
                                  const int32_t* lens, const int32_t* q_lens,

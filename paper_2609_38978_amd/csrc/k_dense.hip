@@ -116,9 +116,13 @@ __global__ __launch_bounds__((FEW ? 64 * dense_few_waves<T, D>() : 256),
   const int qi = r / a.G, hq = hk * a.G + r % a.G;
   int n = a.Nk, p0 = a.q_pos, nq = a.Nq;
   if constexpr (F8) {
-    n = min(max(a.lens[b], 0), a.max_pages << a.page_shift);
+    // (the queries end with the sequence; its keys, where the table does)
+    const int len = max(a.lens[b], 0);
+    n = min(len, a.max_pages << a.page_shift);
     if (a.q_lens) nq = min(max(a.q_lens[b], 0), a.Nq);
-    p0 = n - nq;
+    p0 = len - nq;
+    if (len > n && nq > 0 && a.status && tid == 0 && rt == 0 && hk == 0 && it.part <= 0)
+      atomicOr(a.status, ST_BAD_PAGE);
   }
   const bool exists = r < a.R && qi < nq;
   bool valid = exists;
