@@ -362,13 +362,14 @@ __device__ __forceinline__ uint32_t bit_ne0(int x) { return (uint32_t)(x | -x) >
 
 // ------------------------------------------------------------- score variants
 // The tanh cap of a tile's scores, c = cap tanh(x) with x = scale s / cap, and with
-// GATE its derivative 1 - tanh^2.  Scores are mostly small beside the cap: where
-// all of a wavefront's are (|x| < 5/16) tanh is x (1 + z p(z)), z = x^2, with p of
-// three terms fitted over that range (1.7e-8 off, relative; 4096 float rows at cap
-// 30: 69 -> 63.6 us, and no cancellation); elsewhere it is
-// 1 - 2 r with r = 1 / (1 + e^2x), whose derivative is 4 r (1 - r).  That form's
-// error, about 1e-7, is absolute: float inputs, whose products are exact enough
-// to show it, choose by element.
+// GATE its derivative 1 - tanh^2.  Where |x| < 5/16, tanh is x (1 + z p(z)), z = x^2,
+// with p of three terms fitted over that range (1.7e-8 off, relative); elsewhere it
+// is 1 - 2 r with r = 1 / (1 + e^2x), whose derivative is 4 r (1 - r) and whose error,
+// about 1e-7, is absolute: of a small score under a large cap it would leave little.
+// So each element chooses for itself, also because a masked score, or another row's,
+// is not to change a bit of it.  Scores are mostly small beside the cap: where all of
+// a wavefront's are, the second form is left out (4096 float rows at cap 30:
+// 69 -> 63.6 us).
 __device__ __forceinline__ float tanh_small(float x) {
   const float z = x * x;
   float p = fmaf(z, -0.0500828841f, 0.133117658f);
@@ -380,7 +381,7 @@ __device__ __forceinline__ float dense_tanh(float s, const DenseArgs& a) {
   if (fabsf(s) < a.cap_small) return tanh_small(s * a.cap_arg);
   return fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * a.cap_exp)), 1.0f);
 }
-template <bool F32, bool GATE>
+template <bool GATE>
 __device__ __forceinline__ void dense_cap_tile(f32x16_t& st, const DenseArgs& a, f32x16_t* gate) {
   float top = 0.0f;
 #pragma unroll
@@ -395,17 +396,13 @@ __device__ __forceinline__ void dense_cap_tile(f32x16_t& st, const DenseArgs& a,
   } else {
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
-      const float e = __builtin_amdgcn_exp2f(st[q] * a.cap_exp);
-      const float r = __builtin_amdgcn_rcpf(1.0f + e);
-      float c = fmaf(-2.0f * a.cap, r, a.cap), y = fmaf(-4.0f * r, r, 4.0f * r);
-      if constexpr (F32) {
-        const float t = tanh_small(st[q] * a.cap_arg);
-        const bool small = fabsf(st[q]) < a.cap_small;
-        c = small ? a.cap * t : c;
-        y = small ? fmaf(-t, t, 1.0f) : y;
-      }
-      st[q] = c;
-      if constexpr (GATE) (*gate)[q] = y;
+      float x = st[q];
+      asm volatile("" : "+v"(x));  // (one after the other: all at once spill registers)
+      const float t = tanh_small(x * a.cap_arg);
+      const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * a.cap_exp));
+      const bool small = fabsf(x) < a.cap_small;
+      st[q] = small ? a.cap * t : fmaf(-2.0f * a.cap, r, a.cap);
+      if constexpr (GATE) (*gate)[q] = small ? fmaf(-t, t, 1.0f) : fmaf(-4.0f * r, r, 4.0f * r);
     }
   }
 }

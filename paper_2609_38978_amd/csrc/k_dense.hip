@@ -345,7 +345,7 @@ __global__ __launch_bounds__((FEW ? 64 * dense_few_waves<T, D>() : 256),
   auto finish = [&](auto masked, int t, f32x16_t& st) {
     if constexpr (MOD) {
       if (a.cap > 0.0f) {
-        dense_cap_tile<F32, false>(st, a, nullptr);
+        dense_cap_tile<false>(st, a, nullptr);
       } else {
 #pragma unroll
         for (int q = 0; q < 16; ++q) st[q] *= a.scale;

@@ -145,11 +145,11 @@ __device__ __forceinline__ void lds_dma16_far(const void* p, uint32_t lds) {
 // Score variants on a tile: st becomes the scores in their final units (raw
 // products without variants) and gate the tanh's derivative.  far(q): distance
 // of register q's pair; slope(q) its head's slope.
-template <bool F32, class Far, class Slope>
+template <class Far, class Slope>
 __device__ __forceinline__ void grad_variants(const DenseArgs& a, f32x16_t& st, f32x16_t& gate,
                                               Far far, Slope slope) {
   if (a.cap > 0.0f) {
-    dense_cap_tile<F32, true>(st, a, &gate);
+    dense_cap_tile<true>(st, a, &gate);
   } else {
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
@@ -305,8 +305,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 && D == 128) ? 1
     __builtin_amdgcn_s_setprio(0);
     const float far0 = (float)(pos - 32 * t - 4 * hf);
     if constexpr (MOD)
-      grad_variants<F32>(a, st, gate, [&](int q) { return far0 - (float)(8 * (q >> 2) + (q & 3)); },
-                         [&](int) { return slope; });
+      grad_variants(a, st, gate, [&](int q) { return far0 - (float)(8 * (q >> 2) + (q & 3)); },
+                    [&](int) { return slope; });
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
       const float p = grad_exp<F32>(st[q], x0, sl2);
@@ -528,8 +528,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void k_dense_dkv(con
     __builtin_amdgcn_s_setprio(0);
     if constexpr (MOD) {
       const float far0 = (float)(__float_as_int(field(6, 0)) - j);
-      grad_variants<F32>(a, st, gate, [&](int q) { return far0 + field(4, q); },
-                         [&](int q) { return field(5, q); });
+      grad_variants(a, st, gate, [&](int q) { return far0 + field(4, q); },
+                    [&](int q) { return field(5, q); });
     }
 #pragma unroll
     for (int q = 0; q < 16; ++q) {

@@ -7,7 +7,7 @@ import torch
 import dense_ref as R
 from paper_2609_38978_amd import park as P
 from test_gpu_cache import check_cached, filled, ints, tables
-from test_gpu_dense import rand
+from test_gpu_dense import rand, run
 
 pytestmark = pytest.mark.gpu
 BF, F = torch.bfloat16, torch.float32
@@ -55,3 +55,78 @@ def test_the_longest_length():
     out, lse = torch.full((1, 2, 3, 64), 9.0, device="cuda"), torch.full((1, 2, 3), 9.0, device="cuda")
     P.park_cache_attention(Q, cache, table, ints([2 ** 31 - 1]), out=out, lse=lse)
     check_cached(Q, cache, table, [2 ** 31 - 1], [3], out, lse)
+
+
+def relative_cap(Q, K, V, dO, opts, ok):
+    """R.attention with the bounds of a cap whose tanh is off by 5 roundings (of
+    scale / cap, of the product with it, of the sum x + x z p, of the product with
+    the cap, and of the polynomial: 2^-21 together), relative, for scores far below
+    the cap: those of no cap, and 2^-21 |x| more for each score."""
+    val, tol = R.attention(Q, K, V, dO, **opts)
+    plain = {k: v for k, v in opts.items() if k != "softcap"}
+    tol = R.attention(Q, K, V, dO, **plain)[1]
+    G = Q.shape[1] // K.shape[1]
+    s = Q.shape[-1] ** -0.5 * (Q.double() @ K.double().repeat_interleave(G, 1).transpose(-1, -2))
+    top = torch.where(ok[:, None], s.abs(), 0.0).amax(-1)
+    more = 2 * 2.0 ** -21 * top  # of a probability, relative: its own and its normaliser's
+    vabs = torch.where(ok.any(1)[:, None, :, None], V, 0.0).double().abs().repeat_interleave(G, 1)
+    p = torch.exp(torch.where(ok[:, None], s, -INF) - val["lse"][..., None])
+    p = torch.where(ok[:, None], p, 0.0) * 1.01
+    tol["O"] = tol["O"] + 1.01 * more[..., None] * (p @ vabs)
+    tol["lse"] = tol["lse"] + more
+    return val, tol
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F, 64)])
+@pytest.mark.parametrize("where", ["masked keys", "padded queries"])
+def test_large_scores_beside_small_ones_under_a_large_cap(where, dtype, d):
+    # a key that nobody attends, or a query of no document, with scores about the
+    # cap's size in every tile: the others keep a tanh of relative error
+    gen = torch.Generator(device="cuda").manual_seed(53)
+    B, H, N, cap = 2, 2, 300, 1e6
+    Q, K, V = (rand(gen, B, H, N, d, dtype) for _ in range(3))
+    kd = torch.zeros(B, N, dtype=torch.int32, device="cuda")
+    qd = kd.clone()
+    if where == "masked keys":
+        kd[:, 5::16] = -1
+        K[:, :, 5::16] *= 1e6
+    else:
+        qd[:, 5::16] = -1
+        Q[:, :, 5::16] *= 1e6
+    opts = dict(softcap=cap, q_doc=qd, k_doc=kd)
+    ok = R.allowed(B, N, N, "cuda", q_doc=qd, k_doc=kd)
+    val, tol = relative_cap(*(torch.where((i >= 0)[:, None, :, None], t, 0.0) for t, i in
+                              ((Q, qd), (K, kd), (V, kd))), None, opts, ok)
+    got = run(Q, K, V, None, opts)
+    for n in got:
+        R.check(n, got[n], val[n], tol[n])
+
+
+@pytest.mark.parametrize("Nq", [1, 40])
+def test_large_scores_behind_a_cached_sequence(Nq):
+    # what stands behind the last token (an earlier sequence's, or nothing yet) has
+    # scores about the cap's size
+    gen = torch.Generator(device="cuda").manual_seed(54)
+    table, n = tables(gen, 1, 3)
+    cache = filled(gen, n, 2, 64, 64)
+    T = 70
+    last = int(table[0, 1])
+    cache["k"][last, :, T - 64:] = 0x7e  # 448
+    cache["k_exp"][last] = 0
+    first = cache["k"][last, :, :T - 64].view(R.F8)
+    first.copy_(torch.randn(2, T - 64, 64, generator=gen, device="cuda").to(R.F8))
+    Q = rand(gen, 1, 4, Nq, 64, BF)
+    Q[..., 0] = 500.0
+    cache["k"][..., 0][cache["k"][..., 0] != 0x7e] = 0
+    out, lse = torch.full((1, 4, Nq, 64), 9.0, device="cuda"), torch.full((1, 4, Nq), 9.0, device="cuda")
+    cap = 3e4
+    P.park_cache_attention(Q, cache, table, ints([T]), softcap=cap, out=out, lse=lse)
+    k, v, there = R.cached_kv(cache, table, ints([T]))
+    pos = torch.arange(Nq, device="cuda")[None] + T - Nq
+    ok = there[:, None, :] & (torch.arange(k.shape[2], device="cuda") <= pos[..., None])
+    k, v = (torch.where(there[:, None, :, None], t, 0.0) for t in (k, v))
+    val, tol = relative_cap(Q, k, v, None, dict(softcap=cap, ok=ok, pos=pos), ok)
+    u = R.attention(Q, k, v, ok=ok, pos=pos, u_out=2.0 ** -24)[1]
+    bf = R.attention(Q, k, v, ok=ok, pos=pos)[1]
+    R.check("O", out, val["O"], tol["O"] - bf["O"] + u["O"])
+    R.check("lse", lse, val["lse"], tol["lse"])
