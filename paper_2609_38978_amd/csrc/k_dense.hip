@@ -432,9 +432,12 @@ __global__ __launch_bounds__((FEW ? 64 * dense_few_waves<T, D>() : 256),
   auto step = [&](auto masked, auto sure, int t, const f32x16_t& sc, f32x16_t& sn) {
     arrive(sure, t);
     const uint32_t okc = okn;
-    // the reference moves only when a maximum exceeds it by more than 2^8 in probability
-    if (__any((tmax - m) * sl2 > 8.0f)) {
-      const float mnew = fmaxf(m, tmax);
+    // a row's reference moves only when its maximum exceeds it by more than 2^8 in
+    // probability, whatever the wavefront's other rows do (their contents are not
+    // to change its rounding)
+    const bool up = (tmax - m) * sl2 > 8.0f;
+    if (__any(up)) {
+      const float mnew = up ? tmax : m;
       const float alpha = __builtin_amdgcn_exp2f((m - mnew) * sl2);
       lsum *= alpha;
 #pragma unroll

@@ -130,3 +130,74 @@ def test_large_scores_behind_a_cached_sequence(Nq):
     bf = R.attention(Q, k, v, ok=ok, pos=pos)[1]
     R.check("O", out, val["O"], tol["O"] - bf["O"] + u["O"])
     R.check("lse", lse, val["lse"], tol["lse"])
+
+
+JUNK = (3e4, -2e3, NAN, INF, -INF)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F, 64), (F, 128)])
+@pytest.mark.parametrize("cap", [0.0, 50.0, 1e6])
+@pytest.mark.parametrize("kind", ["padded", "scattered", "few"])
+def test_masked_places_change_no_bit(kind, cap, dtype, d):
+    # whatever stands in tokens of no document, every other row has the same bits
+    gen = torch.Generator(device="cuda").manual_seed(55)
+    B, Hq, Hkv, Nq, Nk = (2, 4, 2, 5, 1500) if kind == "few" else (2, 4, 2, 420, 420)
+    Q, dO = (rand(gen, B, Hq, Nq, d, dtype) * 2 for _ in range(2))
+    K, V = (rand(gen, B, Hkv, Nk, d, dtype) * 2 for _ in range(2))
+    qd, kd = (torch.zeros(B, n, dtype=torch.int32, device="cuda") for n in (Nq, Nk))
+    if kind == "padded":
+        qd[0, 300:], kd[0, 250:], qd[1, 77:], kd[1, 77:] = -1, -1, -1, -1
+    else:
+        qd[:, 3::7], kd[:, 5::11] = -1, -1
+    opts = dict(softcap=cap, q_doc=qd, k_doc=kd)
+    at = lambda i: (i < 0)[:, None, :, None]  # noqa: E731
+    want = run(*(torch.where(at(i), torch.zeros((), dtype=dtype, device="cuda"), t)
+                 for t, i in ((Q, qd), (K, kd), (V, kd), (dO, qd))), opts)
+    for bad in JUNK:
+        x = torch.tensor(bad, dtype=dtype, device="cuda")
+        got = run(*(torch.where(at(i), x, t) for t, i in ((Q, qd), (K, kd), (V, kd), (dO, qd))), opts)
+        for n in want:
+            same = torch.equal(got[n], want[n])
+            assert same, (n, bad)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F, 64), (F, 128)])
+@pytest.mark.parametrize("Nq", [4, 300])
+@pytest.mark.parametrize("cap", [0.0, 6.0])
+def test_a_row_does_not_depend_on_other_queries(cap, Nq, dtype, d):
+    # O, lse and dQ of a row have the same bits beside other queries
+    gen = torch.Generator(device="cuda").manual_seed(56)
+    Q, dO = (rand(gen, 1, 4, Nq, d, dtype) for _ in range(2))
+    K, V = (rand(gen, 1, 2, 1100, d, dtype) for _ in range(2))
+    opts = dict(softcap=cap, causal=True)
+    want = run(Q, K, V, dO, opts)
+    other = torch.arange(Nq, device="cuda") % 3 == 1
+    for size in (0.0, 1.5, 60.0):
+        q = torch.where(other[:, None], rand(gen, 1, 4, Nq, d, dtype, spread=size), Q)
+        got = run(q, K, V, dO, opts)
+        for n in ("O", "lse", "dQ"):
+            same = torch.equal(got[n][:, :, ~other], want[n][:, :, ~other])
+            assert same, (n, size)
+
+
+@pytest.mark.parametrize("Nq", [1, 90])
+@pytest.mark.parametrize("cap", [0.0, 50.0])
+def test_the_rest_of_a_page_changes_no_bit(cap, Nq):
+    gen = torch.Generator(device="cuda").manual_seed(57)
+    B, Hq, Hkv, d, page, mp = 3, 4, 2, 64, 64, 20
+    lens = [1203, 90, 1025]
+    table, n = tables(gen, B, mp)
+    cache = filled(gen, n, Hkv, page, d)
+    Q = rand(gen, B, Hq, Nq, d, BF) * 2
+    behind = torch.zeros(n, page, dtype=torch.bool, device="cuda")
+    for b in range(B):
+        for t in range(mp):
+            behind[int(table[b, t]), max(0, min(page, lens[b] - t * page)):] = True
+    outs = []
+    for byte in (0, 0x7e, 0xfe, 0x7f):
+        for side in ("k", "v"):
+            cache[side][behind[:, None, :, None].expand_as(cache[side])] = byte
+        outs.append(P.park_cache_attention(Q, cache, table, ints(lens), softcap=cap, want_lse=True))
+    for O, lse in outs[1:]:
+        same = torch.equal(O, outs[0][0]) and torch.equal(lse, outs[0][1])
+        assert same
