@@ -86,6 +86,9 @@ struct DenseArgs {
 constexpr float DENSE_NOKEY = -1e30f;
 constexpr int DENSE_ROWS = 128;                // held rows of a workgroup
 constexpr int DENSE_PAGES = 2048;              // pages a workgroup of the cache kernel can hold
+// range of the exponent of a cached page and head, which writing holds to and reading
+// clamps to (448 2^119 is finite, and the smallest e4m3 value's 2^-119 normal, in bf16)
+constexpr int CACHE_EMIN = -110, CACHE_EMAX = 119;
 constexpr int DENSE_MAXSPLIT = 64;
 constexpr int DENSE_FEW = 32;                  // rows of a head that its own form takes
 

@@ -18,8 +18,6 @@
 
 namespace park {
 
-constexpr int CACHE_EMIN = -110, CACHE_EMAX = 119;
-
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
 // eight floats as e4m3 (round to nearest even; NaN for what is not finite)

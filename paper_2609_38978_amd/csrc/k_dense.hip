@@ -231,7 +231,9 @@ __global__ __launch_bounds__((FEW ? 64 * dense_few_waves<T, D>() : 256),
     __syncthreads();
   }
   const bool anybad = F8 && bad_pages;
-  auto exp2i = [](int e) { return __uint_as_float((uint32_t)(min(max(e, -118), 119) + 127) << 23); };
+  auto exp2i = [](int e) {
+    return __uint_as_float((uint32_t)(min(max(e, CACHE_EMIN), CACHE_EMAX) + 127) << 23);
+  };
   auto kscale = [&](int t) {  // power of two of this lane's key row
     if constexpr (F8) return exp2i((int8_t)ptab[((t * 32 + c32) >> a.page_shift) - pbase].y);
     else return 1.0f;

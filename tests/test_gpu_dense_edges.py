@@ -201,3 +201,35 @@ def test_the_rest_of_a_page_changes_no_bit(cap, Nq):
     for O, lse in outs[1:]:
         same = torch.equal(O, outs[0][0]) and torch.equal(lse, outs[0][1])
         assert same
+
+
+@pytest.mark.parametrize("e", [-128, -119, -111, -110, 119, 127])
+@pytest.mark.parametrize("Nq", [2, 50])
+def test_exponents_past_their_range(Nq, e):
+    # a page's exponent is read as if within [-110, 119], of keys and of values
+    gen = torch.Generator(device="cuda").manual_seed(58)
+    d, page = 64, 16
+    c = min(max(e, -110), 119)
+    table = ints([[2, 0, 1]])
+    Q = rand(gen, 1, 2, Nq, d, BF)
+    pos = torch.arange(Nq, device="cuda")[None] + 41 - Nq
+    cache = filled(gen, 3, 1, page, d)
+    e0 = cache["v_exp"].clone()
+    for side in ("v", "k"):
+        cache["v_exp"].copy_(e0)
+        cache["k_exp"].copy_(e0)
+        cache[side + "_exp"].fill_(e)
+        # values q 2^e with q below 2, so that 2^119 q is finite
+        cache[side].copy_(torch.randint(0, 0x40, cache[side].shape, generator=gen, device="cuda"))
+        k, v, there = R.cached_kv(cache, table, ints([41]))
+        ok = there[:, None, :] & (torch.arange(48, device="cuda") <= pos[..., None])
+        unit = cache[side][table.long()].view(R.F8).double().transpose(1, 2).reshape(1, 1, 48, d)
+        out, lse = torch.empty(1, 2, Nq, d, device="cuda"), torch.empty(1, 2, Nq, device="cuda")
+        q = Q if side == "v" else Q * 2.0 ** (-c if c < 0 else -100)  # (bf16: exact)
+        scale = d ** -0.5 * (1.0 if side == "v" or c < 0 else 2.0 ** (100 - c))
+        P.park_cache_attention(q, cache, table, ints([41]), out=out, lse=lse, scale=scale)
+        # (relative to 2^c: the bounds have an absolute 1e-30)
+        val, tol = R.attention(Q, k if side == "v" else unit, unit if side == "v" else v, ok=ok, pos=pos,
+                               u_out=2.0 ** -24)
+        R.check("lse", lse, val["lse"], tol["lse"])
+        R.check("O", out.double() * (2.0 ** -c if side == "v" else 1.0), val["O"], tol["O"])
