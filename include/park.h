@@ -414,7 +414,8 @@ park_status park_attention(const park_rows* Q, const park_rows* K, const park_ro
  * not depend on the order in which workgroups run.  With bf16 inputs the
  * probabilities and the scores' gradients are rounded to bf16 before their
  * products, and each row's sum dO . O is formed from O as it was stored (but
- * for rows that see the first 8 keys at the most, which form it anew): an O of
+ * for rows of at most 8 keys that are the first of all or within 8 places of
+ * the row's own, as in a short document of a pack: those form it anew): an O of
  * float (out_dtype) leaves it exact. */
 park_status park_attention_backward(const park_rows* dO, const park_rows* Q, const park_rows* K,
                                     const park_rows* V, const park_rows* O, const float* lse,

@@ -35,9 +35,12 @@ namespace park {
 // so, which the sums of dS spread over a row's keys; where there are few the
 // difference dP - D is small and shows it (causal texts of 2 and 4 tokens: dQ and
 // dK 0.01 and 0.0046 off in norm; 0.0032 and 0.0028 with D from its definition,
-// sum_j P_ij dP_ij).  Rows whose keys are all among the first DENSE_NEAR take that
-// (16 instead of 8: 0.0025 instead of 0.0027 at 16 tokens, but 90 instead of 53 us
-// for 64 x 24 heads of 256 tokens, 37 without).
+// sum_j P_ij dP_ij).  Rows that attend at most DENSE_NEAR keys take that if those
+// are the first of all, or within DENSE_NEAR places of the row's own as those of a
+// short document in a pack are.  It costs 14 us of the kernel's 51 for 64 x 24
+// causal heads of 256 tokens, d = 128 (16 keys: 53, for 0.0025 instead of 0.0027 at
+// 16 tokens), and of packs of 2 x 24 heads of 8192 tokens 12 us of 54, 18 of 60 and
+// 55 of 97 where documents have 256, 32 and 4.
 constexpr int DENSE_NEAR = 8;
 
 // exp(x - lse) for a score x in the kernel's units, sl2 = log2(e) in them: one
@@ -48,20 +51,39 @@ __device__ __forceinline__ float grad_exp(float x, float x0, float sl2) {
   return __builtin_amdgcn_exp2f(F32 ? (x + x0) * sl2 : fmaf(x, sl2, x0));
 }
 
-// elements part E .. part E + E - 1 of a row
+// elements part E .. part E + E - 1 of a row as they are stored
 template <class T, int E>
-__device__ __forceinline__ void load_part(const char* p, int part, float (&y)[E]) {
+struct RowPart {
+  static constexpr int W = sizeof(T) == 4 ? E : E / 2;
+  alignas(16) uint32_t w[W];
+  __device__ __forceinline__ RowPart(const char* p, int part) {
+    p += part * (E * (int)sizeof(T));
 #pragma unroll
-  for (int e = 0; e < E; e += 4) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 u = *(const float4*)(p + (part * E + e) * 4);
-      y[e] = u.x, y[e + 1] = u.y, y[e + 2] = u.z, y[e + 3] = u.w;
-    } else {
-      const uint2 u = *(const uint2*)(p + (part * E + e) * 2);
-      y[e] = bf2f((bf16_t)u.x), y[e + 1] = bf2f((bf16_t)(u.x >> 16));
-      y[e + 2] = bf2f((bf16_t)u.y), y[e + 3] = bf2f((bf16_t)(u.y >> 16));
-    }
+    for (int e = 0; e < W; e += 4) *(uint4*)(w + e) = *(const uint4*)(p + 4 * e);
   }
+  __device__ __forceinline__ float operator[](int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else return bf2f((bf16_t)(w[e / 2] >> 16 * (e & 1)));
+  }
+};
+template <int E, class A, class B>
+__device__ __forceinline__ float dot_part(const A& a, const B& b) {
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) s = fmaf(a[e], b[e], s);
+  return s;
+}
+
+// ... of two rows of one type: bf16 in pairs (the products exact, sums in float)
+template <class T, int E>
+__device__ __forceinline__ float dot_rows(const RowPart<T, E>& a, const RowPart<T, E>& b) {
+  if constexpr (sizeof(T) == 4) return dot_part<E>(a, b);
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < E / 2; ++e)
+    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, a.w[e]),
+                                        __builtin_bit_cast(bf16x2_t, b.w[e]), s, false);
+  return s;
 }
 
 template <class T, class OT, int D>
@@ -73,18 +95,15 @@ __global__ __launch_bounds__(256) void k_dense_rows(const DenseArgs a, const Den
   float x0 = -INFINITY, dd = 0.0f, slope = 0.0f;
   int jlim = -1, doc = -1;
   const int pos = qi + a.q_pos;
+  const size_t at = ((size_t)b * a.Hkv * a.G + hq) * a.Nq + qi;  // (r < R)
+  // documents of the 17 keys around the row's own place, one or two a lane
+  const int base = max(min(pos, a.Nk - 1) - DENSE_NEAR, 0);
+  int id[3] = {-1, -1, -1};
   if (r < a.R) {
     const char* o = a.o.p + b * a.o.b + hq * a.o.h + qi * a.o.r;
     const char* dout = g.dout.p + b * g.dout.b + hq * g.dout.h + qi * g.dout.r;
     constexpr int E = D / 8;
-    {
-      float y[E], z[E];
-      load_part<T, E>(dout, part, y);
-      load_part<OT, E>(o, part, z);
-#pragma unroll
-      for (int e = 0; e < E; ++e) dd = fmaf(y[e], z[e], dd);
-    }
-    const size_t at = ((size_t)b * a.Hkv * a.G + hq) * a.Nq + qi;
+    dd = dot_part<E>(RowPart<T, E>(dout, part), RowPart<OT, E>(o, part));
     const float lse = g.lse[at];
     x0 = lse == INFINITY ? NAN : -lse * unit;
     if (lse == -INFINITY) x0 = -INFINITY;
@@ -92,39 +111,60 @@ __global__ __launch_bounds__(256) void k_dense_rows(const DenseArgs a, const Den
     if (a.causal) jlim = min(jlim, max(pos, a.prefix ? a.prefix[b] - 1 : -1));
     if (a.q_doc) {
       doc = a.q_doc[(size_t)b * a.Nq + qi];
+      if constexpr (sizeof(OT) == 2) {
+        const int* ids = a.k_doc + (size_t)b * a.Nk;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)  // (past the last: the last, which `ok` leaves out)
+          id[i] = ids[min(base + DENSE_NEAR * i + (i < 2 ? part : 0), a.Nk - 1)];
+      }
       if (doc < 0) jlim = -1;
     }
     if (a.slopes) slope = a.slopes[hq];
-    if (sizeof(OT) == 2 && jlim >= 0 && jlim < DENSE_NEAR) {
-      const float sl2 = (a.cap > 0.0f || a.slopes ? 1.0f : a.scale) * 1.4426950408889634f;
-      const char* kp = a.k.p + b * a.k.b + hk * a.k.h;
-      const char* vp = a.v.p + b * a.v.b + hk * a.v.h;
-      float q[E], y[E];
-      load_part<T, E>(a.q.p + b * a.q.b + hq * a.q.h + qi * a.q.r, part, q);
-      load_part<T, E>(dout, part, y);
-      dd = 0.0f;
-#pragma unroll 1  // (few rows come here: registers for the others' loads)
-      for (int i = 0; i <= jlim; ++i) {
-        float k[E], v[E];
-        load_part<T, E>(kp + i * a.k.r, part, k);
-        load_part<T, E>(vp + i * a.v.r, part, v);
-        const bool ok = !a.q_doc || a.k_doc[(size_t)b * a.Nk + i] == doc;
-        float x = 0.0f, dp = 0.0f;
+  }
+  if constexpr (sizeof(OT) == 2) {
+    // the keys of the row among the 17, as bits
+    static_assert(DENSE_NEAR == 8, "eight lanes a row");
+    uint32_t keys = jlim >= 0 && jlim < DENSE_NEAR ? (2u << jlim) - 1u : 0u;
+    bool all = true;  // it has no others
+    if (a.q_doc) {
+      keys = 0u;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          x = fmaf(q[e], k[e], x);
-          dp = fmaf(y[e], v[e], dp);
-        }
+      for (int i = 0; i < 3; ++i) {
+        const bool ok = id[i] == doc && base + DENSE_NEAR * i + (i < 2 ? part : 0) <= jlim;
+        keys |= ((uint32_t)(__ballot(ok) >> (threadIdx.x & 56)) & (i < 2 ? 255u : 1u)) << (8 * i);
+      }
+      if (__builtin_popcount(keys) > DENSE_NEAR) keys = 0u;
+      all = base == 0 && jlim <= 2 * DENSE_NEAR;
+    }
+    if (keys) {
+      const float sl2 = (a.cap > 0.0f || a.slopes ? 1.0f : a.scale) * 1.4426950408889634f;
+      const int j0 = a.q_doc ? base : 0;
+      const char* kp = a.k.p + b * a.k.b + hk * a.k.h + j0 * a.k.r;
+      const char* vp = a.v.p + b * a.v.b + hk * a.v.h + j0 * a.v.r;
+      constexpr int E = D / 8;
+      const RowPart<T, E> q(a.q.p + b * a.q.b + hq * a.q.h + qi * a.q.r, part);
+      const RowPart<T, E> y(g.dout.p + b * g.dout.b + hq * g.dout.h + qi * g.dout.r, part);
+      float near = 0.0f, psum = 0.0f;
+#pragma unroll 1  // (few rows come here: registers for the others' loads)
+      for (; keys; keys &= keys - 1) {
+        const int i = __builtin_ctz(keys);
+        const RowPart<T, E> k(kp + i * a.k.r, part), v(vp + i * a.v.r, part);
+        float x = dot_rows(q, k);
+        const float dp = dot_rows(y, v);
 #pragma unroll
         for (int s = 4; s > 0; s >>= 1) x += __shfl_xor(x, s, 8);
         if (a.cap > 0.0f) x = a.cap * dense_tanh(x, a);
         else if (a.slopes) x *= a.scale;
-        x = fmaf(-slope, (float)abs(pos - i), x);
-        if (ok) dd = fmaf(grad_exp<sizeof(T) == 4>(x, x0, sl2), dp, dd);
+        x = fmaf(-slope, (float)abs(pos - j0 - i), x);
+        const float p = grad_exp<sizeof(T) == 4>(x, x0, sl2);
+        psum += p;
+        near = fmaf(p, dp, near);
       }
+      // (elsewhere it may have others: what those weigh is what these lack)
+      if (all || psum > 1.0f - 0x1p-11f) dd = near;
     }
-    if (g.dlse && part == 0) dd -= g.dlse[at];
   }
+  if (g.dlse && part == 0 && r < a.R) dd -= g.dlse[at];
 #pragma unroll
   for (int s = 4; s > 0; s >>= 1) dd += __shfl_xor(dd, s, 8);
   const int first = 32 * t / a.G + a.q_pos;

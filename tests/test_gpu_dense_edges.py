@@ -233,3 +233,91 @@ def test_exponents_past_their_range(Nq, e):
                                u_out=2.0 ** -24)
         R.check("lse", lse, val["lse"], tol["lse"])
         R.check("O", out.double() * (2.0 ** -c if side == "v" else 1.0), val["O"], tol["O"])
+
+
+def few_keys(Q, K, V, dO, ok, cap):
+    """dQ, dK and their bounds where D is formed from its definition: what is left is
+    the rounding of dS and of the result (2^-8 each) and float sums (d + 16 roundings
+    of 2^-24 of P (|dO||v| + sum P |dO||v|), and as much for P's own)."""
+    B, Hq, Nq, d = Q.shape
+    Hkv, Nk = K.shape[1:3]
+    ok = ok[:, None]
+    q, g = Q.double(), dO.double()
+    k, v = (t.double().repeat_interleave(Hq // Hkv, 1) for t in (K, V))
+    s = d ** -0.5 * (q @ k.transpose(-1, -2))
+    t = torch.tanh(s / cap) if cap else torch.zeros_like(s)
+    x = torch.where(ok, cap * t if cap else s, -INF)
+    p = torch.where(ok, torch.exp(x - torch.logsumexp(x, -1, keepdim=True)), 0.0)
+    dp, mag = g @ v.transpose(-1, -2), g.abs() @ v.abs().transpose(-1, -2)
+    ds = p * (dp - (p * dp).sum(-1, keepdim=True)) * (1 - t * t)
+    # scores are off by d 2^-24 |q||k| scale (and 4e-7 of the cap): so is P, relative
+    size = torch.where(ok, q.abs() @ k.abs().transpose(-1, -2), 0.0).amax(-1, keepdim=True)
+    es = 2 * (d + 16) * 2.0 ** -24 * (1 + d ** -0.5 * size) + (8e-7 * cap if cap else 0.0)
+    eds = 2.0 ** -8 * ds.abs() + (2 * es + (d + 16) * 2.0 ** -22) * p * (mag + (p * mag).sum(-1, keepdim=True))
+    heads = lambda y: y.view(B, Hkv, Hq // Hkv, Nk, d).sum(2)  # noqa: E731
+    dq, edq = d ** -0.5 * (ds @ k), d ** -0.5 * (eds @ k.abs())
+    dk, edk = (d ** -0.5 * heads(y) for y in (ds.transpose(-1, -2) @ q, eds.transpose(-1, -2) @ q.abs()))
+    return (dq, edq * 1.01 + 2.0 ** -8 * dq.abs() + 1e-30), (dk, edk * 1.01 + 2.0 ** -8 * dk.abs() + 1e-30)
+
+
+def check_few(Q, K, V, dO, opts, rows=None, keys=None):
+    B, Nq, Nk = Q.shape[0], Q.shape[2], K.shape[2]
+    got = run(Q, K, V, dO, opts)
+    ok = R.allowed(B, Nq, Nk, "cuda", **{k: v for k, v in opts.items() if k != "softcap"})
+    (dq, eq), (dk, ek) = few_keys(Q, K, V, dO, ok, opts.get("softcap"))
+    r = slice(None) if rows is None else rows
+    c = slice(None) if keys is None else keys
+    R.check("dQ", got["dQ"][:, :, r], dq[:, :, r], eq[:, :, r])
+    R.check("dK", got["dK"][:, :, c], dk[:, :, c], ek[:, :, c])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [1, 2, 3, 4, 7, 8])
+def test_gradients_of_short_documents_anywhere(size, d):
+    # documents of a few tokens at every place of a pack
+    gen = torch.Generator(device="cuda").manual_seed(59)
+    B, Hq, Hkv, N = 2, 6, 2, 333
+    Q, dO = (rand(gen, B, Hq, N, d, BF) for _ in range(2))
+    K, V = (rand(gen, B, Hkv, N, d, BF) for _ in range(2))
+    ids = (torch.arange(N, device="cuda", dtype=torch.int32) // size).expand(B, N).contiguous()
+    for more in (dict(causal=True), dict(softcap=20.0), dict(causal=True, prefix=ints([40, 333])), {}):
+        check_few(Q, K, V, dO, dict(q_doc=ids, k_doc=ids, **more))
+
+
+def test_gradients_of_documents_in_pieces():
+    # a document of which a row sees a few keys around its own place and others far
+    # away (in front of it, or behind): D is not that of the near ones alone
+    gen = torch.Generator(device="cuda").manual_seed(65)
+    Q, K, V, dO = (rand(gen, 1, 2, 400, 64, BF) for _ in range(4))
+    ids = torch.arange(400, device="cuda", dtype=torch.int32) % 100 // 5
+    for more in (dict(causal=True), {}):
+        opts = dict(q_doc=ids[None].contiguous(), k_doc=ids[None].contiguous(), **more)
+        got = run(Q, K, V, dO, opts)
+        val, tol = R.attention(Q, K, V, dO, **opts)
+        for n in got:
+            R.check(n, got[n], val[n], tol[n])
+
+
+@pytest.mark.parametrize("N", [700, 9000])
+def test_gradients_of_short_documents_after_a_long_one(N):
+    gen = torch.Generator(device="cuda").manual_seed(60)
+    Hq, Hkv, d = (4, 2, 64) if N < 1000 else (1, 1, 64)
+    Q, dO = (rand(gen, 1, Hq, N, d, BF) for _ in range(2))
+    K, V = (rand(gen, 1, Hkv, N, d, BF) for _ in range(2))
+    long = N - 101
+    ids = torch.cat([torch.zeros(long, device="cuda"), 1 + torch.arange(101, device="cuda") // 4]).int()[None]
+    short = torch.arange(long, N, device="cuda")
+    for more in (dict(causal=True), {}):
+        check_few(Q, K, V, dO, dict(q_doc=ids, k_doc=ids, **more), short, short)
+
+
+def test_gradients_of_queries_with_few_keys_of_their_own():
+    # keys and queries of different counts: eight keys of each query's document
+    gen = torch.Generator(device="cuda").manual_seed(61)
+    B, Hq, Hkv, Nq, Nk, d = 2, 3, 1, 150, 400, 128
+    Q, dO = (rand(gen, B, Hq, Nq, d, BF) for _ in range(2))
+    K, V = (rand(gen, B, Hkv, Nk, d, BF) for _ in range(2))
+    kd = (torch.arange(Nk, device="cuda", dtype=torch.int32) // 8).expand(B, Nk).contiguous()
+    qd = torch.randint(-1, 55, (B, Nq), generator=gen, device="cuda", dtype=torch.int32)
+    check_few(Q, K, V, dO, dict(q_doc=qd, k_doc=kd))
+    check_few(Q, K, V, dO, dict(q_doc=qd, k_doc=kd, causal=True))
