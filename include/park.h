@@ -380,7 +380,7 @@ typedef struct park_attn_dims {
  * Scores below -1e30 count as -infinity. */
 typedef struct park_attn_opts {
   double scale;          /* > 0, at most 2^20 (1 / sqrt(d) as a rule)           */
-  double softcap;        /* > 0, or 0 for none                                  */
+  double softcap;        /* 1e-30 .. 1e30 (at most 2^126 scale), or 0 for none  */
   const float* slopes;   /* [Hq] device, or NULL                                */
   int32_t causal;        /* 0 or 1                                              */
   int32_t q_pos;         /* position of query 0 among the keys, |q_pos| < 2^30

@@ -94,6 +94,8 @@ static park_status check_opts(const park_attn_opts* o, int Nq, int Nk) {
     return fail(PARK_ERR_INVALID_ARG, "scale %g must be in [1e-30, 2^20]", o->scale);
   if (o->softcap != 0.0 && !(o->softcap >= 1e-30 && o->softcap <= 1e30))
     return fail(PARK_ERR_INVALID_ARG, "softcap %g must be 0 or in [1e-30, 1e30]", o->softcap);
+  if (o->softcap > o->scale * 0x1p126)  // (scale / softcap is a float of its full precision)
+    return fail(PARK_ERR_INVALID_ARG, "softcap %g is above 2^126 scale (%g)", o->softcap, o->scale);
   if (o->causal != 0 && o->causal != 1)
     return fail(PARK_ERR_INVALID_ARG, "causal = %d must be 0 or 1", o->causal);
   if (o->q_pos <= -(1 << 30) || o->q_pos >= (1 << 30))
