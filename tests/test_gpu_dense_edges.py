@@ -321,3 +321,53 @@ def test_gradients_of_queries_with_few_keys_of_their_own():
     qd = torch.randint(-1, 55, (B, Nq), generator=gen, device="cuda", dtype=torch.int32)
     check_few(Q, K, V, dO, dict(q_doc=qd, k_doc=kd))
     check_few(Q, K, V, dO, dict(q_doc=qd, k_doc=kd, causal=True))
+
+
+@pytest.mark.parametrize("side", ["k", "v"])
+@pytest.mark.parametrize("byte", [0x7f, 0xff])
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64)])
+@pytest.mark.parametrize("Nq", [1, 150])
+def test_attended_nan_of_a_cache_is_seen(Nq, d, page, byte, side):
+    # in a whole tile, in a partial one at the end, and where a causal limit falls;
+    # the longest sequence is read in parts
+    gen = torch.Generator(device="cuda").manual_seed(62)
+    B, Hq, Hkv, lens = 3, 4, 2, [6001, 205, 400]
+    table, n = tables(gen, B, -(-6001 // page) + 1)
+    cache = filled(gen, n, Hkv, page, d)
+    Q = rand(gen, B, Hq, Nq, d, BF)
+    places = [(0, 0, 70, 3), (0, 1, 5998, d - 1), (1, 0, 204, 0), (1, 1, 130, 17), (2, 0, 0, 33)]
+    for b, h, j, c in places:
+        cache[side][int(table[b, j // page]), h, j % page, c] = byte
+    O, lse = P.park_cache_attention(Q, cache, table, ints(lens), want_lse=True, out_dtype=F)
+    want_o = torch.zeros(B, Hq, Nq, d, dtype=torch.bool, device="cuda")
+    want_l = torch.zeros(B, Hq, Nq, dtype=torch.bool, device="cuda")
+    for b, h, j, c in places:
+        sees = torch.arange(Nq, device="cuda") + lens[b] - Nq >= j
+        for hq in (2 * h, 2 * h + 1):
+            want_o[b, hq] |= sees[:, None] & ((torch.arange(d, device="cuda") == c) if side == "v" else True)
+            want_l[b, hq] |= sees & (side == "k")
+    assert torch.equal(O.isnan(), want_o) and torch.equal(lse.isnan(), want_l)
+    # and what is beside them is right
+    k, v, there = R.cached_kv(cache, table, ints(lens))
+    k, v = k.nan_to_num(0.0), v.nan_to_num(0.0)
+    for b in range(B):
+        pos = torch.arange(Nq, device="cuda")[None] + lens[b] - Nq
+        ok = there[b][None, None] & (torch.arange(k.shape[2], device="cuda") <= pos[..., None])
+        val, tol = R.attention(Q[b:b + 1], k[b:b + 1], v[b:b + 1], ok=ok, pos=pos, u_out=2.0 ** -24)
+        f = ~want_o[b:b + 1]
+        R.check("O", O[b:b + 1][f], val["O"][f], tol["O"][f])
+
+
+@pytest.mark.parametrize("dtype", [BF, F], ids=["bf16", "f32"])
+def test_a_nan_appended_is_attended(dtype):
+    # from the input through the pages to the output
+    gen = torch.Generator(device="cuda").manual_seed(63)
+    table, n = tables(gen, 1, 4)
+    cache = P.make_kv_cache(n, 1, 32, 64)
+    K, V = (rand(gen, 1, 1, 100, 64, dtype) for _ in range(2))
+    V[0, 0, 40, 7], V[0, 0, 90, 9] = INF, NAN
+    P.park_cache_append(cache, K, V, table, ints([0]))
+    O = P.park_cache_attention(rand(gen, 1, 1, 100, 64, BF), cache, table, ints([100]))[0, 0]
+    assert O[40:, 7].isnan().all() and O[90:, 9].isnan().all()
+    O[40:, 7], O[90:, 9] = 0.0, 0.0
+    assert O.isfinite().all()
