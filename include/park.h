@@ -447,7 +447,8 @@ typedef struct park_kv_cache {
  * n_new NULL: N each).  The exponent of a page and head is the smallest e in
  * [-110, 119] with |x| <= 448 2^e for its finite elements so far; in a page
  * that holds older tokens it may rise, and their values are then rounded to it.
- * Rounding is to the nearest, ties to even; NaN and infinities become NaN.
+ * Rounding is to the nearest, ties to even; NaN, infinities and what rounds to
+ * more than 448 2^119 become NaN.
  * Tokens whose page id is not valid are left out.  lens and the table are not
  * changed.  The pages that a call writes must be distinct (a page shared by
  * two sequences is copied before either appends to it). */

@@ -20,7 +20,8 @@ namespace park {
 
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// eight floats as e4m3 (round to nearest even; NaN for what is not finite)
+// eight floats as e4m3 (round to nearest even; NaN for what is not finite or rounds
+// past 448)
 __device__ __forceinline__ uint2 to_f8(const float* x, float s) {
   uint32_t w[2];
 #pragma unroll

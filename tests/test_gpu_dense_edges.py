@@ -6,7 +6,7 @@ import torch
 
 import dense_ref as R
 from paper_2609_38978_amd import park as P
-from test_gpu_cache import check_cached, filled, ints, tables
+from test_gpu_cache import check_cached, filled, ints, same_pages, tables
 from test_gpu_dense import rand, run
 
 pytestmark = pytest.mark.gpu
@@ -371,3 +371,20 @@ def test_a_nan_appended_is_attended(dtype):
     assert O[40:, 7].isnan().all() and O[90:, 9].isnan().all()
     O[40:, 7], O[90:, 9] = 0.0, 0.0
     assert O.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F], ids=["bf16", "f32"])
+def test_append_at_the_end_of_the_range(dtype):
+    # 448 2^119 is the largest value a page holds; what rounds to more becomes NaN,
+    # as infinities do, and leaves its neighbours alone
+    x = torch.zeros(1, 1, 2, 64)
+    x[0, 0, 0, :11] = torch.tensor([448.0, 456.0, 464.0, 472.0, 480.0, 508.0, -464.0, -472.0, 440.0, 100.0, 2.0])
+    x[0, 0, 1, :3] = torch.tensor([0.015625, 2.0 ** -9, 2.0 ** -10])  # normal, subnormal, half of that: to even
+    x = (x.double() * 2.0 ** 119).to(dtype).cuda()
+    assert x.isfinite().all()
+    cache = P.make_kv_cache(1, 1, 16, 64)
+    want = R.append(cache, x, -x, torch.tensor([[0]]), [0], [2])
+    P.park_cache_append(cache, x, -x, ints([[0]]), ints([0]))
+    same_pages(cache, want)
+    nan = cache["k"][0, 0, 0, :11].view(R.F8).float().isnan().tolist()
+    assert nan == [False] * 3 + [True] * 3 + [False, True] + [False] * 3
