@@ -12,8 +12,9 @@
 //
 // Bound by the matrix cores (8 heads of 16384 tokens, d = 128: dQ 1.4 ms =
 // 1.16 PFLOP/s for its three products, dK and dV 1.9 ms = 1.14 for their four; the
-// forward beside them 1.0 ms), with cap and bias by vector instructions (2 x 16
-// heads of 4133 rows in 5 documents: dQ 94 us, dK and dV 151).
+// forward beside them 1.0 ms).  With documents of different lengths by their parts'
+// uneven work and, with cap and bias, by vector instructions (2 x 16 heads of 4133
+// rows in 5 documents: dQ 102 us, dK and dV 177, the CUs at work half of that).
 #include <math.h>
 
 #include <algorithm>

@@ -456,6 +456,10 @@ def park_attention(Q, K, V, *, scale=None, softcap: float = 0.0, slopes=None,
     position of query 0 among the keys, Nk - Nq), prefix [B] int32 (causal only)
     and the documents q_doc [B, Nq], k_doc [B, Nk] int32 are park_attn_opts of
     include/park.h.  O has Q's dtype unless out or out_dtype says otherwise.
+
+    As everywhere here autograd sees nothing of the call: O carries no history,
+    whatever Q, K and V require.  The gradient is park_attention_backward, which a
+    torch.autograd.Function's backward can call with what its forward kept.
     """
     q = _view(Q, "Q")
     Hkv, Nk = (K.shape[-3], K.shape[-2]) if K.dim() == Q.dim() else (0, 0)

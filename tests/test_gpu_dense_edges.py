@@ -388,3 +388,33 @@ def test_append_at_the_end_of_the_range(dtype):
     same_pages(cache, want)
     nan = cache["k"][0, 0, 0, :11].view(R.F8).float().isnan().tolist()
     assert nan == [False] * 3 + [True] * 3 + [False, True] + [False] * 3
+
+
+def test_gradients_inside_an_autograd_function():
+    # outputs carry no history of their own; a Function that keeps what the gradient
+    # takes gives autograd the same gradients as the call itself
+    gen = torch.Generator(device="cuda").manual_seed(66)
+    opts = dict(causal=True, softcap=20.0)
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v):
+            O, lse = P.park_attention(q, k, v, want_lse=True, **opts)
+            ctx.save_for_backward(q, k, v, O, lse)
+            return O, lse
+
+        @staticmethod
+        def backward(ctx, dO, dlse):
+            return P.park_attention_backward(dO.contiguous(), *ctx.saved_tensors, dlse=dlse.contiguous(), **opts)
+
+    Q, w = (rand(gen, 2, 4, 130, 64, BF) for _ in range(2))
+    K, V = (rand(gen, 2, 2, 130, 64, BF) for _ in range(2))
+    leaves = [t.clone().requires_grad_() for t in (Q, K, V)]
+    assert not P.park_attention(*leaves, **opts).requires_grad
+    O, lse = Attention.apply(*leaves)
+    ((O * w).sum() + 2 * lse.sum()).backward()
+    o, l = P.park_attention(Q, K, V, want_lse=True, **opts)  # noqa: E741
+    want = P.park_attention_backward(w, Q, K, V, o, l, dlse=torch.full_like(l, 2.0), **opts)
+    for t, g in zip(leaves, want):
+        same = torch.equal(t.grad, g)
+        assert same
