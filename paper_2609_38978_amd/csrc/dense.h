@@ -371,8 +371,8 @@ __device__ __forceinline__ uint32_t bit_ne0(int x) { return (uint32_t)(x | -x) >
 // about 1e-7, is absolute: of a small score under a large cap it would leave little.
 // So each element chooses for itself, also because a masked score, or another row's,
 // is not to change a bit of it.  Scores are mostly small beside the cap: where all of
-// a wavefront's are, the second form is left out (4096 float rows at cap 30:
-// 69 -> 63.6 us).
+// a wavefront's are, the second form is left out (16 causal bf16 heads of 4096 rows,
+// d = 64: 109 us at cap 50, 139 at cap 3, where no tile can; the gradient 306 and 375).
 __device__ __forceinline__ float tanh_small(float x) {
   const float z = x * x;
   float p = fmaf(z, -0.0500828841f, 0.133117658f);
@@ -397,15 +397,22 @@ __device__ __forceinline__ void dense_cap_tile(f32x16_t& st, const DenseArgs& a,
       if constexpr (GATE) (*gate)[q] = fmaf(-t, t, 1.0f);
     }
   } else {
+    // (a number of its own: what both branches compute would be moved before them,
+    // where it spills registers)
+    float arg = a.cap_arg;
+    asm volatile("" : "+s"(arg));
+    // (both forms, then the choice: the compiler would branch for each element)
+    auto choose = [](bool first, float x, float y) {
+      asm("" : "+v"(x), "+v"(y));
+      return first ? x : y;
+    };
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
-      float x = st[q];
-      asm volatile("" : "+v"(x));  // (one after the other: all at once spill registers)
-      const float t = tanh_small(x * a.cap_arg);
-      const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * a.cap_exp));
-      const bool small = fabsf(x) < a.cap_small;
-      st[q] = small ? a.cap * t : fmaf(-2.0f * a.cap, r, a.cap);
-      if constexpr (GATE) (*gate)[q] = small ? fmaf(-t, t, 1.0f) : fmaf(-4.0f * r, r, 4.0f * r);
+      const float t = tanh_small(st[q] * arg);
+      const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(st[q] * a.cap_exp));
+      const bool small = fabsf(st[q]) < a.cap_small;
+      st[q] = choose(small, a.cap * t, fmaf(-2.0f * a.cap, r, a.cap));
+      if constexpr (GATE) (*gate)[q] = choose(small, fmaf(-t, t, 1.0f), fmaf(-4.0f * r, r, 4.0f * r));
     }
   }
 }
